@@ -89,6 +89,8 @@ __device__ __forceinline__ uint32_t f16_bits(float f) {
     return __builtin_bit_cast(uint16_t, h);
 }
 
+__device__ __forceinline__ _Float16 f16_of(uint32_t bits) { return __builtin_bit_cast(_Float16, (uint16_t)bits); }
+
 __device__ __forceinline__ void widen_octet(const uint4& raw, int dt, float (&x)[8]) {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
@@ -119,7 +121,10 @@ __device__ __forceinline__ uint32_t quantise(const uint4& raw, int dt, uint32_t&
     const float s = f16_bits_to_f32(sb);
     const uint32_t cb = f16_bits(lo - kKv4Bias * s);
     const float c = f16_bits_to_f32(cb);
-    bad = (sb & 0x7C00u) == 0x7C00u || (cb & 0x7C00u) == 0x7C00u;
+    // What the largest code stands for, as attention forms it: no number of fp16 where that is none, nor where s or c is (an infinite s
+    // makes c infinite with the other sign).  No code stands for less than c, so an infinity can only be this one.
+    const _Float16 top = __builtin_elementwise_fma((_Float16)(kKv4Bias + 15.f), f16_of(sb), f16_of(cb));
+    bad = (__builtin_bit_cast(uint16_t, top) & 0x7C00u) == 0x7C00u;
     scales = sb | (cb << 16);
     // 1 / s correctly rounded: one step from the hardware's, whose error it squares to 2^-46, and no quotient of an 11-bit s lies within
     // 2^-36 of the middle between two floats

@@ -1,0 +1,113 @@
+"""The 4-bit key/value cache at the ends of its ranges: values near and past fp16's largest."""
+import numpy as np
+import pytest
+import torch
+
+import kv4_plain as plain
+import paper_2412_07174_amd as scap
+from test_gpu_kv4 import BF, F, Cache, i32
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ values that fp16 has not
+def top_is_a_number(s, c):
+    """Whether what code 15 stands for is a number of fp16: 79 s + c is exact in fp64 (18 bits of a product and 11 more, not 2^15 apart
+    where it matters), so the conversion is the one rounding."""
+    with np.errstate(all="ignore"):
+        return np.isfinite((79 * s.astype(np.float64) + c.astype(np.float64)).astype(np.float16)).all(-1)
+
+
+def token_codes(k, v):
+    """plain.token_codes with the last condition."""
+    qk, sk, ck, a = plain.quantise(k)
+    qv, sv, cv, b = plain.quantise(v)
+    bad = ~(a & b & top_is_a_number(sk, ck) & top_is_a_number(sv, cv))
+    for q in (qk, qv):
+        q[bad] = 0
+    for s in (sk, ck, sv, cv):
+        s.view(np.uint16)[bad] = 0x7E00
+    return qk, sk, ck, qv, sv, cv
+
+
+# ends of a group; what is readable of it is token_codes' to say
+ENDS = {BF: [(60000, 66000), (90000, 105000), (70400, 86900), (64000, 65000), (65280, 65280), (-105000, -90000), (-65280, -64000), (0, 15000),
+             (-7000, 65280)],
+        F: [(63648, 65504), (50144, 65504), (65504, 65504), (60000, 60100), (65440, 65504), (-65504, -63648), (-65504, -65504), (0, 15350)]}
+
+
+def near_the_end(dt, n, heads, D, seed):
+    """Tokens [n, heads, D] whose first group lies between ends such as these, or anywhere near them; the others are ordinary."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, heads, D), generator=g)
+    t = torch.rand((n, heads, 32), generator=g)
+    t[..., 0], t[..., 1] = 0, 1
+    for i in range(n):
+        for h in range(heads):
+            if i < len(ENDS[dt]):
+                lo, hi = ENDS[dt][i]
+            else:
+                hi = 65504 - 60 * float(torch.rand((), generator=g)) if dt == F else 40000 + 70000 * float(torch.rand((), generator=g))
+                lo = hi - 16000 * float(torch.rand((), generator=g)) ** 2
+            x[i, h, :32] = lo + t[i, h] * (hi - lo)
+    return x.to(dt)
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("D,P,n", [(64, 16, 300), (128, 64, 300), (128, 32, 2100)])
+def test_append_of_values_that_fp16_has_not(dt, D, P, n, monkeypatch):
+    """Bit for bit: unreadable where code 15 stands for no number of fp16, as before otherwise."""
+    heads = 2
+    c = Cache([n], heads, D, P, dt, seed=D)
+    c.k[0][:300], c.v[0][-300:] = near_the_end(dt, 300, heads, D, 1), near_the_end(dt, 300, heads, D, 2)
+    c.fill_all()
+    monkeypatch.setattr(plain, "token_codes", token_codes)
+    want = plain.Pool(c.pages, heads, D, P)
+    for pos in range(n):
+        want.put(c.table[0, pos // P], pos % P, c.k[0][pos].float().numpy(), c.v[0][pos].float().numpy())
+    assert np.array_equal(c.cache.pool[0].cpu().numpy(), want.bytes)
+    held = np.isfinite(c.stood_for(0)[0]).all(-1)
+    assert 2 < (~held).sum() < 2 * n - 10, "both kinds occur"
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_gives_what_the_cache_holds_near_the_end_of_fp16(dt, D, monkeypatch):
+    """Sequences of one token, whose probability is 1: its value, rounded to fp16 by the widening and to the output's type, bit for bit;
+    NaN where it cannot be read."""
+    n, heads = 400, 2
+    c = Cache([1] * n, heads, D, 16, dt, seed=5)
+    x = near_the_end(dt, n, heads, D, 3)
+    for b in range(n):
+        c.v[b] = x[b:b + 1]
+    c.fill_all()
+    monkeypatch.setattr(plain, "token_codes", token_codes)
+    ws = scap.KV4Workspace(c.cache, seqs=n, tokens=n, heads=4, max_new=1)
+    q = torch.zeros((n, 4, D), dtype=dt, device="cuda")
+    got = scap.kv4_attention(c.cache, q, i32(range(n + 1)), c.d_table, c.d_lens, max_new=1, workspace=ws).cpu()
+    want = np.stack([c.stood_for(b)[1][0] for b in range(n)]).repeat(2, 1)
+    unreadable = np.isnan(want)
+    assert 2 < unreadable.any((1, 2)).sum() < n - 10, "both kinds occur"
+    want = torch.from_numpy(want.astype(np.float16)).to(dt)
+    assert np.array_equal(got.isnan().numpy(), unreadable) and torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("dt,lo,hi", [(BF, 70400, 86900), (BF, 60000, 66000), (F, 63648, 65504)])
+@pytest.mark.parametrize("n,heads,window", [(5, 8, 0), (5, 8, 2), (70, 8, 0), (70, 8, 3), (280, 128, 0), (280, 128, 2)])
+@pytest.mark.parametrize("where", ["k", "v"])
+def test_a_finite_token_past_fp16_reaches_only_who_sees_it(dt, lo, hi, n, heads, window, where):
+    """At the edge of what rows see: those before it, and those whose window has passed it, get the bits they get without it."""
+    outs = []
+    for large in (False, True):
+        c = Cache([300, 90], 2, 128, 64, dt, seed=8)
+        bad = 300 - n + 3
+        if large:
+            (c.k if where == "k" else c.v)[0][bad, 1, 32:64] = torch.linspace(lo, hi, 32).to(dt)
+        c.fill_all()
+        q = torch.randn((n + 1, heads, 128), generator=torch.Generator().manual_seed(1)).to(dt).cuda()
+        ws = scap.KV4Workspace(c.cache, seqs=2, tokens=n + 1, heads=heads)
+        outs.append(scap.kv4_attention(c.cache, q, i32([0, n, n + 1]), c.d_table, c.d_lens, window=window, workspace=ws).cpu())
+    sees = torch.zeros((n + 1, heads), dtype=torch.bool)
+    sees[3:min(3 + window, n) if window else n, heads // 2:] = True   # the upper half of the heads reads kv head 1
+    assert bool(outs[1][sees].isnan().all())
+    assert torch.equal(outs[1][~sees], outs[0][~sees]) and not bool(outs[0].isnan().any())
