@@ -81,6 +81,7 @@ struct Kv4AttnArgs {
     float* partial;
     int64_t slot_floats;  // floats of one workgroup's partial result
     int slot_rows;        // a sequence with more rows is not cut into chunks
+    uint32_t partial_bytes;  // what lies at `partial`: accesses beyond are dropped
 };
 
 int launch_kv4_append(const Kv4TokensArgs& a, hipStream_t stream);

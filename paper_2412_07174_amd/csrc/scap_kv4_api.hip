@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include "scap_kv4.hpp"
+#include "scap_kv4_split.hpp"
 
 using namespace scap;
 
@@ -11,7 +12,7 @@ constexpr int64_t kMaxPages = (int64_t)1 << 24;
 constexpr int64_t kMaxLayerBytes = ((int64_t)1 << 36) - 16;
 constexpr int64_t kMaxSeqs = (int64_t)1 << 20;
 constexpr int64_t kMaxNew = (int64_t)1 << 22;
-constexpr int64_t kMaxRowTokens = (int64_t)1 << 30;
+constexpr int64_t kMaxRowTokens = kKv4MaxRange;
 constexpr int64_t kMaxGroups = ((int64_t)1 << 23) - 1;  // workgroups of up to 512 threads: fewer than 2^32 threads
 constexpr size_t kCounterBytes = (size_t)1 << 20;    // arrival counters at the start of a workspace
 
@@ -175,6 +176,8 @@ int scap_kv4_attention(const scap_kv4_cache* cache, int64_t layer, const void* q
     a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
     a.slot_floats = plan.slot_floats;
     a.slot_rows = plan.slot_rows;
+    const size_t room = workspace_bytes - kCounterBytes;
+    a.partial_bytes = room < 0xFFFFFFFFu ? (uint32_t)room : 0xFFFFFFFFu;
     return launch_kv4_attention(a, plan, static_cast<hipStream_t>(stream));
 }
 

@@ -20,6 +20,7 @@
 
 #include "scap_gemv_parts.hpp"
 #include "scap_kv4.hpp"
+#include "scap_kv4_split.hpp"
 
 namespace scap {
 
@@ -188,14 +189,8 @@ __device__ __forceinline__ bool find_work(const Kv4AttnArgs& a, Work& w) {
         for (int base = 0; base < a.s.B; base += kWave)
             if (body(base, base == 0 ? first : load(base + lane))) break;
     };
-    // (rows that a slot of the workspace does not hold: one chunk; with one place there are no slots, and past 2^24 tokens a chunk of
-    // "all" of them, from a sum in fp32, may lack a few)
     const auto cut = [&](const Seq& q, int chunk, float inv) {
-        if (a.places <= 1 || q.sp.n * a.G > a.slot_rows) return 1;
-        int c = (int)((float)q.range * inv);
-        c += (int64_t)c * chunk < q.range;
-        c -= (int64_t)(c - 1) * chunk >= q.range;
-        return max(c, 1);
+        return kv4_cut(q.range, q.sp.n * a.G, chunk, inv, a.places, a.slot_rows);
     };
     float total = 0.f;  // work, in rows' blocks times tokens
     int n = 0;
@@ -204,23 +199,15 @@ __device__ __forceinline__ bool find_work(const Kv4AttnArgs& a, Work& w) {
         n += last_lane(dpp_scan(q.blocks));
         return false;
     });
-    // Chunks of c tokens make at most total / c + n workgroups of every head, and n / 2 fewer as a rule.  As many as run at once are wanted, and
-    // not a few more, which would run alone behind them: the shortest chunk of three that keeps to that.
-    const int places = max(a.places, 1);
-    int chunk = 0;
     float inv = 0.f;
-    for (int spare = 0; spare < 3; ++spare) {
-        const int left = places - n * spare / 2;
-        if (spare > 0 && left <= 0) break;  // more rows' blocks than places: several rounds in any case
-        chunk = max(a.min_chunk, (int)fminf(total / (float)left + 1.f, 1e9f));
-        inv = 1.f / (float)chunk;
+    const int chunk = kv4_choose_chunk(total, n, max(a.places, 1), a.min_chunk, inv, [&](int chunk, float inv) {
         int items = 0;
         each([&](int, const Seq& q) {
             items += last_lane(dpp_scan(q.blocks * cut(q, chunk, inv)));
             return false;
         });
-        if (items <= places) break;
-    }
+        return items;
+    });
     int item = blockIdx.x / heads, slots = 0, counters = 0;
     w.head = blockIdx.x - item * heads;
     bool found = false;
@@ -604,7 +591,7 @@ struct Partial {
     __amdgpu_buffer_rsrc_t r;
     uint32_t base, ml;  // bytes
     __device__ __forceinline__ Partial(const Kv4AttnArgs& a, int slot)
-        : r(make_raw_buffer(a.partial, 0xFFFFFFFFu)),
+        : r(make_raw_buffer(a.partial, a.partial_bytes)),
           base((uint32_t)(slot * a.slot_floats * 4)),
           ml(base + (uint32_t)(a.slot_floats / (D + 2) * D * 4)) {}
     __device__ __forceinline__ void put(int row, int d, float4 v) const { store_coherent16(r, base + (row * D + d) * 4, v); }
@@ -956,9 +943,7 @@ Kv4AttnPlan plan_kv4_attention(int D, int kv_heads, int64_t B, int64_t T, int G,
     p.staged = staged;
     p.min_chunk = p.rt == 1 ? kMinChunk1 : kMinChunk2;
     // Row blocks of all sequences, at most: one each, and one more per 256 rows (staged; two each up to 64 rows) or per wavefront's rows.
-    // Chunks hold at least 1 / places of a head's work (find_work), so they add at most that many workgroups; rows that are cut have more
-    // than a chunk, so fewer than `places` of them arrive at counters, with at most 2 * places partial results.  With one place nothing
-    // is cut.
+    // What the chunks add to them, and what room they need: scap_kv4_split.hpp.
     const int64_t block_rows = staged ? kStagedWaves * rows : rows;
     const int64_t blocks = (staged ? 2 * B : B) + T * G / block_rows;
     p.waves = staged ? kStagedWaves : (p.rt == 1 ? B * kv_heads < kFewSets1 : blocks * kv_heads <= kFewSets2) ? 8 : 4;
