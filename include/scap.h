@@ -45,7 +45,8 @@ typedef enum {
     SCAP_ERR_SHAPE = -2,     /* a size out of range, or N not a multiple of the vector width */
     SCAP_ERR_DTYPE = -3,     /* unknown dtype / estimator code, or a combination not supported */
     SCAP_ERR_ALIGN = -4,     /* a device pointer is not 16-byte aligned */
-    SCAP_ERR_VALUE = -5,     /* tau negative or NaN, m not finite, target sparsity outside [0, 1); a scale <= 0, a window without causal */
+    SCAP_ERR_VALUE = -5,     /* tau negative or NaN, m not finite, target sparsity outside [0, 1); a scale <= 0, a window without causal,
+                              arrays that may not overlap */
     SCAP_ERR_WORKSPACE = -6, /* workspace NULL or smaller than scap_workspace_bytes() */
     SCAP_ERR_HIP = -7,       /* a HIP runtime call or launch reported an error */
     SCAP_ERR_UNIMPL = -8,    /* valid request that this build does not implement */
@@ -403,7 +404,8 @@ int scap_kv4_reserve(const scap_kv4_cache* cache, int32_t* table, int64_t S, int
 /*
  * ASYNC.  Rows that share all pages of their parents: row j of table_out [B_out, S] is row parents[j] of table [B_in, S] up to
  * its length (-1 behind it), lens_out[j] its length; an empty row where parents[j] is not one of 0 .. B_in - 1.  Every entry counts in
- * refs.  table_out must not overlap the rows that are read, and what it held is not released (scap_kv4_free).
+ * refs.  What table_out held is not released (scap_kv4_free).  table_out and lens_out overlap neither what is read (table, lens, parents) nor each
+ * other (SCAP_ERR_VALUE).
  */
 int scap_kv4_fork(const scap_kv4_cache* cache, const int32_t* table, const int32_t* lens, int64_t B_in, const int32_t* parents,
                   int64_t B_out, int32_t* table_out, int32_t* lens_out, int64_t S, void* stream);

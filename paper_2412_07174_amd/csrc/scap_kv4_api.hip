@@ -18,6 +18,12 @@ constexpr size_t kCounterBytes = (size_t)1 << 20;    // arrival counters at the 
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// whether n words at a and m at b have one in common
+bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + 4 * (uintptr_t)m && y < x + 4 * (uintptr_t)n;
+}
+
 int log2_of(int v) {
     for (int i = 0; i < 31; ++i)
         if (v == 1 << i) return i;
@@ -203,6 +209,12 @@ int scap_kv4_fork(const scap_kv4_cache* cache, const int32_t* table, const int32
     if (rc == SCAP_OK) rc = check_rows(*cache, table_out, S, B_out);
     if (rc != SCAP_OK) return rc;
     if (!aligned(lens, 4) || !aligned(parents, 4) || !aligned(lens_out, 4)) return SCAP_ERR_ALIGN;
+    // a row's length and pages are written while other workgroups still read theirs
+    const int64_t in = B_in * S, out = B_out * S;
+    if (overlap(table_out, out, table, in) || overlap(table_out, out, lens, B_in) || overlap(table_out, out, parents, B_out) ||
+        overlap(lens_out, B_out, table, in) || overlap(lens_out, B_out, lens, B_in) || overlap(lens_out, B_out, parents, B_out) ||
+        overlap(table_out, out, lens_out, B_out))
+        return SCAP_ERR_VALUE;
     return launch_kv4_fork(pool_of(*cache), table, lens, (int)B_in, parents, (int)B_out, table_out, lens_out, (int)S,
                            static_cast<hipStream_t>(stream));
 }

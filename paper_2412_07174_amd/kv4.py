@@ -286,7 +286,7 @@ def kv4_reserve(cache: KV4Cache, table, old_lens, new_lens, *, info: Optional[to
 
 def kv4_fork(cache: KV4Cache, table, lens, parents, table_out, lens_out, *, stream=None) -> None:
     """Row j of table_out shares the pages of row parents[j] of table (none where that is no row); lens_out[j] is its length.  Release
-    what table_out's rows held first (kv4_free)."""
+    what table_out's rows held first (kv4_free).  table_out and lens_out are memory of their own: nothing that is read."""
     _cache_ok(cache)
     dev = cache.dev
     if not (_plain_table(table, dev) and _plain_table(table_out, dev) and _plain_list(lens, table.shape[:1], dev)
@@ -302,10 +302,13 @@ def kv4_fork(cache: KV4Cache, table, lens, parents, table_out, lens_out, *, stre
     B_out, S_out = table_out.shape
     if S_out != S:
         raise ValueError(f"table_out: rows of {S_out} pages, table has {S}")
-    at, at_out = table.data_ptr(), table_out.data_ptr()
-    if at < at_out + 4 * B_out * S and at_out < at + 4 * B * S:
-        raise ValueError("table_out: overlaps table")
-    _call(FORK, cache.at, at, lens.data_ptr(), B, parents.data_ptr(), B_out, at_out, lens_out.data_ptr(), S, _stream(stream))
+    try:
+        _call(FORK, cache.at, table.data_ptr(), lens.data_ptr(), B, parents.data_ptr(), B_out, table_out.data_ptr(), lens_out.data_ptr(), S,
+              _stream(stream))
+    except ScapError as e:
+        if e.status != -5:
+            raise
+        raise ValueError("table_out and lens_out: overlap table, lens or parents, or each other") from None
 
 
 def kv4_free(cache: KV4Cache, table, keep_from=None, keep_to=None, *, stream=None) -> None:

@@ -111,3 +111,24 @@ def test_a_finite_token_past_fp16_reaches_only_who_sees_it(dt, lo, hi, n, heads,
     sees[3:min(3 + window, n) if window else n, heads // 2:] = True   # the upper half of the heads reads kv head 1
     assert bool(outs[1][sees].isnan().all())
     assert torch.equal(outs[1][~sees], outs[0][~sees]) and not bool(outs[0].isnan().any())
+
+
+# ------------------------------------------------------------------------------------------------ pages
+def test_a_fork_refuses_arrays_that_it_reads_and_takes_their_neighbours():
+    cache = scap.KV4Cache(8, 1, 64, page_tokens=16)
+    ints = i32(range(64))
+    table, lens, parents, kids, kid_lens = ints[:6].view(2, 3), ints[6:8], ints[8:11], ints[11:20].view(3, 3), ints[20:23]
+    table.copy_(i32([[5, 6, 7], [2, -1, -1]]))
+    lens.copy_(i32([40, 3]))
+    parents.copy_(i32([1, 0, 1]))
+    before = ints.cpu()
+    for out in (lens.view(-1), parents):
+        n = out.shape[0]
+        with pytest.raises(ValueError):
+            scap.kv4_fork(cache, table, lens, parents[:n], kids[:n], out)
+    with pytest.raises(ValueError):
+        scap.kv4_fork(cache, table, lens, parents, ints[3:12].view(3, 3), kid_lens)
+    assert torch.equal(ints.cpu(), before) and int(cache.refs.sum()) == 0
+    scap.kv4_fork(cache, table, lens, parents, kids, kid_lens)   # side by side is apart
+    assert kid_lens.tolist() == [3, 40, 3] and kids.tolist() == [[2, -1, -1], [5, 6, 7], [2, -1, -1]]
+    assert cache.refs.tolist() == [0, 0, 2, 0, 0, 1, 1, 1]
