@@ -412,8 +412,8 @@ int scap_kv4_fork(const scap_kv4_cache* cache, const int32_t* table, const int32
 
 /*
  * ASYNC.  Releases the pages of B rows that hold no token of [keep_from[b], keep_to[b]): entries become -1, refs drop.
- * keep_from, keep_to  DEVICE int32 [B] or NULL (= 0): both NULL releases whole rows; keep_to = the new length cuts the end;
- * keep_from = length - window lets go of what a window has passed.
+ * keep_from, keep_to  DEVICE int32 [B] or NULL.  Both NULL releases whole rows.  keep_to alone cuts the end: keep_from is 0, keep_to the new
+ * length.  keep_from alone lets go of what a window has passed: keep_from = length - window, everything from there on is kept.
  */
 int scap_kv4_free(const scap_kv4_cache* cache, int32_t* table, int64_t S, int64_t B, const int32_t* keep_from,
                   const int32_t* keep_to, void* stream);

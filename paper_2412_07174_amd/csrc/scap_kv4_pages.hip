@@ -293,7 +293,8 @@ __global__ __launch_bounds__(256) void kv4_free_kernel(Kv4Pool p, int32_t* table
                                                    const int32_t* keep_to) {
     const int per = (S + 255) / 256, row = blockIdx.x / per, s = blockIdx.x % per * 256 + threadIdx.x;
     if (s >= S) return;
-    const int64_t from = keep_from ? keep_from[row] : 0, to = keep_to ? keep_to[row] : 0;
+    // a first token alone keeps all from there on
+    const int64_t from = keep_from ? keep_from[row] : 0, to = keep_to ? keep_to[row] : keep_from ? (int64_t)S << p.lgP : 0;
     const int64_t at = (int64_t)s << p.lgP;
     if (from < to && at < to && at + p.P > from) return;  // holds a kept token
     const int64_t i = (int64_t)row * S + s;

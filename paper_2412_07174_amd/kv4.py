@@ -312,7 +312,8 @@ def kv4_fork(cache: KV4Cache, table, lens, parents, table_out, lens_out, *, stre
 
 
 def kv4_free(cache: KV4Cache, table, keep_from=None, keep_to=None, *, stream=None) -> None:
-    """Releases the pages of table's rows that hold no token of [keep_from, keep_to): whole rows by default."""
+    """Releases the pages of table's rows that hold no token of [keep_from, keep_to): whole rows by default.  keep_to alone keeps
+    the tokens before it, keep_from alone those from there on."""
     _cache_ok(cache)
     if not (keep_from is None and keep_to is None and _plain_table(table, cache.dev)):
         a = _Args()

@@ -132,3 +132,18 @@ def test_a_fork_refuses_arrays_that_it_reads_and_takes_their_neighbours():
     scap.kv4_fork(cache, table, lens, parents, kids, kid_lens)   # side by side is apart
     assert kid_lens.tolist() == [3, 40, 3] and kids.tolist() == [[2, -1, -1], [5, 6, 7], [2, -1, -1]]
     assert cache.refs.tolist() == [0, 0, 2, 0, 0, 1, 1, 1]
+
+
+@pytest.mark.parametrize("keep_from,keep_to", [([0, 1, 16, 17], None), ([40, 63, 64, 200], None), ([-5, 0, 48, 47], None),
+                                               (None, [0, 1, 16, 17]), (None, [40, 63, 64, 200]), (None, [-3, 0, 1000, 33])])
+def test_free_with_one_bound_keeps_what_lies_on_its_side(keep_from, keep_to):
+    P, S = 16, 4
+    cache = scap.KV4Cache(16, 1, 64, page_tokens=P)
+    rows = np.arange(16, dtype=np.int32).reshape(4, S)
+    table = i32(rows)
+    cache.refs.fill_(1)
+    scap.kv4_free(cache, table, **{k: i32(v) for k, v in (("keep_from", keep_from), ("keep_to", keep_to)) if v is not None})
+    first, end = keep_from or [0] * 4, keep_to or [S * P] * 4
+    kept = np.array([[bool(set(range(s * P, (s + 1) * P)) & set(range(first[b], end[b]))) for s in range(S)] for b in range(4)])
+    assert np.array_equal(table.cpu().numpy(), np.where(kept, rows, -1))
+    assert np.array_equal(cache.refs.cpu().numpy().reshape(4, S), kept.astype(np.int32))
