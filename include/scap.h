@@ -437,18 +437,20 @@ int scap_kv4_copy_pages(const scap_kv4_cache* from, const scap_kv4_cache* to, co
 
 /*
  * The calls above with their arguments in order in an array, one 64-bit word each (integers and pointers as they are, the scale of
- * scap_kv4_attention as the bits of the float): for bindings to which every argument of a foreign call costs something.  `what` is one of
- * scap_kv4_what (SCAP_ERR_VALUE otherwise); words HOST.
+ * scap_kv4_attention as the bits of the float): for bindings to which every argument of a foreign call costs something.  words HOST.
+ * `what` is SCAP_KV4_WORDS(one of scap_kv4_what, the number of words); a number that is not the call's is SCAP_ERR_VALUE, before any word is
+ * read, and so is another call.  Without a number the array has to hold what the call takes: it is not known to be shorter.
  */
 typedef enum {
-    SCAP_KV4_APPEND = 0,
-    SCAP_KV4_READ = 1,
-    SCAP_KV4_ATTENTION = 2,
-    SCAP_KV4_RESERVE = 3,
-    SCAP_KV4_FORK = 4,
-    SCAP_KV4_FREE = 5,
-    SCAP_KV4_COMPACT = 6
+    SCAP_KV4_APPEND = 0,    /* 16 words */
+    SCAP_KV4_READ = 1,      /* 12 */
+    SCAP_KV4_ATTENTION = 2, /* 22 */
+    SCAP_KV4_RESERVE = 3,   /* 10 */
+    SCAP_KV4_FORK = 4,      /* 10 */
+    SCAP_KV4_FREE = 5,      /* 7 */
+    SCAP_KV4_COMPACT = 6    /* 10 */
 } scap_kv4_what;
+#define SCAP_KV4_WORDS(what, n) ((what) | (n) << 8)
 int scap_kv4_call(int what, const int64_t* words);
 
 #ifdef __cplusplus

@@ -257,6 +257,10 @@ int scap_kv4_copy_pages(const scap_kv4_cache* from, const scap_kv4_cache* to, co
 
 int scap_kv4_call(int what, const int64_t* w) {
     if (!w) return SCAP_ERR_NULL;
+    static constexpr int kWords[] = {16, 12, 22, 10, 10, 7, 10};
+    const int n = what >> 8;
+    what &= 0xFF;
+    if (n < 0 || what > SCAP_KV4_COMPACT || (n != 0 && n != kWords[what])) return SCAP_ERR_VALUE;
     const auto ptr = [&](int i) { return reinterpret_cast<void*>(static_cast<uintptr_t>(w[i])); };
     const auto ints = [&](int i) { return static_cast<int32_t*>(ptr(i)); };
     const auto cache = static_cast<const scap_kv4_cache*>(ptr(0));

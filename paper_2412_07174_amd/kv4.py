@@ -149,7 +149,8 @@ def _call(what: int, *words) -> None:
     global _entry
     if _entry is None:
         _entry = load_library().scap_kv4_call
-    rc = _entry(what, _pack[len(words)](*words))
+    n = len(words)
+    rc = _entry(what | n << 8, _pack[n](*words))   # SCAP_KV4_WORDS: the entry knows how many each call takes
     if rc != 0:
         raise ScapError(rc, "scap_kv4_" + _NAMES[what])
 

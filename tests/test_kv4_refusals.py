@@ -26,3 +26,14 @@ def test_a_fork_writes_nothing_that_it_reads(out, other, where):
     at[out] = at[other] + {"same": 0, "first word": -4 * (SIZES[out] - 1), "last word": 4 * (SIZES[other] - 1)}[where]
     lib = scap.load_library()
     assert lib.scap_kv4_fork(cache(), at["table"], at["lens"], 6, at["parents"], 4, at["table_out"], at["lens_out"], 5, None) == -5
+
+
+@pytest.mark.parametrize("what,n", enumerate([16, 12, 22, 10, 10, 7, 10]))
+def test_a_packed_call_of_another_number_of_words_reads_none(what, n):
+    """A number that is not the call's is refused before the array is touched (its address here is nowhere); the call's own goes on to
+    the cache, which is missing."""
+    lib = scap.load_library()
+    for wrong in (1, n - 1, n + 1, 255, 1 << 20):
+        assert lib.scap_kv4_call(what | wrong << 8, ctypes.c_char_p(8)) == -5
+    assert lib.scap_kv4_call(what | n << 8, bytes(8 * n)) == -1
+    assert lib.scap_kv4_call(7 | n << 8, ctypes.c_char_p(8)) == -5 and lib.scap_kv4_call(what - (1 << 8), ctypes.c_char_p(8)) == -5
