@@ -375,7 +375,8 @@ int scap_kv4_read(const scap_kv4_cache* cache, int64_t layer, void* k_out, void*
  * ASYNC.  Attention of the new tokens' queries over the cache, one launch:
  *     out[t, h] = sum_j softmax_j(scale * q[t, h] . k_j) v_j     over the positions j that token t, at position p, sees:
  * j < lens[b], and where causal j <= p, and where window > 0 j > p - window (window > 0 needs causal).  Query head h reads
- * kv head h / (heads / kv_heads).  A token that sees nothing gets 0.  Append first: a token's own position counts.
+ * kv head h / (heads / kv_heads).  A token that sees nothing gets 0; a query with a NaN or
+ * an infinity that sees something gets NaN.  Append first: a token's own position counts.
  *   q          DEVICE  dtype dt; strides as in scap_kv4_append.
  *   heads      query heads, a multiple of kv_heads.
  *   max_new    the most new tokens of a sequence, 0 if not known: a hint that picks the faster kernel; results are right without it.

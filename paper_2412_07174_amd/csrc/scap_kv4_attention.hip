@@ -243,7 +243,8 @@ __device__ __forceinline__ bool find_work(const Kv4AttnArgs& a, Work& w) {
 }
 
 // One row tile's queries: lane (row = lane & 15, quarter) holds the channels that it holds of a key, in the order in which widening
-// leaves them, times 2^-e with e the exponent of the row's largest.  back: 2^e.
+// leaves them, times 2^-e with e the exponent of the row's largest.  back: 2^e.  A row with an infinity is NaN throughout: its scores are
+// infinite or NaN, their softmax is NaN in either case, and scores of -infinity alone would look like a row that sees nothing.
 template <int D>
 __device__ __forceinline__ void load_queries(const Kv4AttnArgs& a, const Work& w, int row, bool live, Frag* q, float& back) {
     constexpr int KW = D / 32;
@@ -268,7 +269,7 @@ __device__ __forceinline__ void load_queries(const Kv4AttnArgs& a, const Work& w
     const uint32_t ex = most >> 23;
     const bool scaled = most != 0 && ex < 255;
     const uint32_t e = min(max(ex, 1u), 253u);
-    const float f = scaled ? __uint_as_float((254u - e) << 23) : 1.f;
+    const float f = scaled ? __uint_as_float((254u - e) << 23) : most == 0 ? 1.f : __builtin_nanf("");
     back = scaled ? __uint_as_float(e << 23) : 1.f;
 #pragma unroll
     for (int o = 0; o < KW; ++o)

@@ -147,3 +147,34 @@ def test_free_with_one_bound_keeps_what_lies_on_its_side(keep_from, keep_to):
     kept = np.array([[bool(set(range(s * P, (s + 1) * P)) & set(range(first[b], end[b]))) for s in range(S)] for b in range(4)])
     assert np.array_equal(table.cpu().numpy(), np.where(kept, rows, -1))
     assert np.array_equal(cache.refs.cpu().numpy().reshape(4, S), kept.astype(np.int32))
+
+
+# ------------------------------------------------------------------------------------------------ queries
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("D,n,heads", [(64, 1, 4), (128, 5, 8), (128, 70, 8), (128, 280, 128), (64, 200, 64)])
+@pytest.mark.parametrize("x", [float("inf"), float("-inf"), float("nan")])
+def test_a_query_that_is_no_number_gives_none(dt, D, n, heads, x):
+    """Whatever the signs of what it meets: an infinite score less the maximum is none either.  Other rows get the bits they get without it,
+    and one that sees nothing is empty all the same."""
+    c = Cache([300, 90], 2, D, 64, dt, seed=8)
+    c.k[0][:, 0, 5] = c.k[0][:, 0, 5].abs() + 0.5     # x times this has one sign for the first half of the heads
+    c.k[0][:, 0, 6] = -c.k[0][:, 0, 6].abs() - 0.5
+    c.fill_all()
+    starts = i32([0, n, n + 2])
+    ws = scap.KV4Workspace(c.cache, seqs=2, tokens=n + 2, heads=heads)
+    q = torch.randn((n + 2, heads, D), generator=torch.Generator().manual_seed(1)).to(dt).cuda()
+    c.d_table[1] = -1                                 # the second sequence's pages are missing
+    outs = []
+    bad = torch.zeros((n + 2, heads), dtype=torch.bool)
+    for put in (False, True):
+        if put:
+            for t in (0, n // 2, n):
+                for h in (0, heads // 2 - 1, heads // 2):
+                    q[t, h, 5 + t % 2] = x
+                    bad[t, h] = t < n
+        lse = torch.empty((n + 2, heads), device="cuda")
+        outs.append((scap.kv4_attention(c.cache, q, starts, c.d_table, c.d_lens, lse=lse, workspace=ws).cpu(), lse.cpu()))
+    (want, want_lse), (got, got_lse) = outs
+    assert bool(got[bad].isnan().all()) and bool(got_lse[bad].isnan().all())
+    assert torch.equal(got[~bad], want[~bad]) and torch.equal(got_lse[~bad], want_lse[~bad])
+    assert bool((got[n:] == 0).all()) and not bool(want.isnan().any())
