@@ -380,7 +380,7 @@ int scap_kv4_read(const scap_kv4_cache* cache, int64_t layer, void* k_out, void*
  *   q          DEVICE  dtype dt; strides as in scap_kv4_append.
  *   heads      query heads, a multiple of kv_heads.
  *   max_new    the most new tokens of a sequence, 0 if not known: a hint that picks the faster kernel; results are right without it.
- *   scale      finite and > 0.
+ *   scale      finite and > 0.  Scores scale * q . k may have any size that fp32 holds (times log2 e).
  *   out        DEVICE  [T, heads, D], dtype dt, 16-byte aligned.  Rows of tokens that belong to no sequence are not written.
  *   lse        DEVICE  fp32 [T, heads] or NULL: log of the sum of exp(scale * q . k_j); -inf where nothing is seen.
  *   workspace  scap_kv4_workspace_bytes(cache, B, T, heads, max_new) bytes, initialised.

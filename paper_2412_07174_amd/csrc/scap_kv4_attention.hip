@@ -39,7 +39,10 @@ constexpr int kTile = 32;        // tokens a wavefront takes at a time
 constexpr int kMinChunk1 = 128, kMinChunk2 = 256;
 constexpr float kShift = 10.f;   // probabilities are held times 2^kShift ...
 constexpr float kSlack = 5.f;    // ... and the running maximum is moved only when it is passed by more than 2^kSlack
-constexpr float kNone = -1e30f;  // maximum of nothing (finite: 2^(-inf - kNone) is 0 and no NaN)
+constexpr float kNone = -3.402823466e38f;  // maximum of nothing (finite: 2^(-inf - kNone) is 0 and no NaN)
+// From this size of a maximum on, scores are rounded before it is taken off.  One fma, which is cheaper, takes it off the exact product: the maximum's
+// own probability is then 2^(its rounding) instead of 1, which below is 1 in fp16 and from 2^23 on would be past its range or 0.
+constexpr float kFar = 4096.f;
 
 __device__ __forceinline__ h2_t as_h2(uint32_t u) { return __builtin_bit_cast(h2_t, u); }
 __device__ __forceinline__ uint32_t as_u32(h2_t h) { return __builtin_bit_cast(uint32_t, h); }
@@ -286,6 +289,8 @@ struct State {
     f4_t o[RT][D / 16];
     f4_t l[RT];     // sum of the probabilities, in every element; kept current in [0] only
     float m[RT];    // running maximum (base 2)
+    float past[RT]; // what a score has to pass for it to be moved: kSlack above, any score where it is far
+    float w[RT], base[RT];  // a probability is 2^(w score + base)
     float a[RT];    // score -> base-2 logarithm
     int lo[RT], hi[RT];  // what my row of the tile sees
 };
@@ -371,16 +376,16 @@ __device__ __forceinline__ void scores(const State<D, RT>& st, const Frag (&k)[D
     }
 }
 
-// The state brought up to the maximum of N times 16 tokens' scores.
+// The state brought up to the maximum of N times 16 tokens' scores.  Those of rows whose maximum is far become what is left above it.
 template <int D, int RT, int N>
-__device__ __forceinline__ void raise(State<D, RT>& st, int r, const f4_t (&s)[N][RT]) {
+__device__ __forceinline__ void raise(State<D, RT>& st, int r, f4_t (&s)[N][RT]) {
     float most = s[0][r][0];
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) most = fmaxf(most, s[n][r][e]);
     most *= st.a[r];
-    if (__ballot(most > st.m[r] + kSlack) != 0) {
+    if (__ballot(most > st.past[r]) != 0) {
         most = fmaxf(most, __shfl_xor(most, 16, kWave));
         most = fmaxf(most, __shfl_xor(most, 32, kWave));
         const float m = fmaxf(st.m[r], most);
@@ -389,21 +394,31 @@ __device__ __forceinline__ void raise(State<D, RT>& st, int r, const f4_t (&s)[N
         st.l[r][0] *= f;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) st.o[r][i] *= f;
+        const bool far = fabsf(m) >= kFar && m != kNone;
+        st.past[r] = far ? -__builtin_inff() : m + kSlack;
+        st.base[r] = far ? kShift : kShift - m;
+        st.w[r] = far ? 1.f : st.a[r];
+        if (__ballot(far) != 0) {
+#pragma clang fp contract(off)
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][r][e] = far ? s[n][r][e] * st.a[r] - m : s[n][r][e];
+        }
     }
 }
 
 // Probabilities of one row tile and 32 tokens.
 template <int D, int RT>
 __device__ __forceinline__ Frag probabilities(const State<D, RT>& st, int r, const f4_t& s0, const f4_t& s1) {
-    const float base = kShift - st.m[r];
     Frag p;
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const f4_t& s = half ? s1 : s0;
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * e], st.a[r], base));
-            const float y = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], st.a[r], base));
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * e], st.w[r], st.base[r]));
+            const float y = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], st.w[r], st.base[r]));
             p.h[2 * half + e] = h2_t{(_Float16)x, (_Float16)y};
         }
     return p;
@@ -645,7 +660,8 @@ __global__ __launch_bounds__(WAVES * kWave, RT == 1 ? kOcc1 : kOcc2) void kv4_at
             st.a[r] = a.scale * back;
             const Rows mine = rows_of(a, w.span, live ? row : 0, live ? 1 : 0);
             st.lo[r] = mine.lo, st.hi[r] = mine.hi;
-            st.m[r] = kNone;
+            st.m[r] = st.past[r] = kNone;
+            st.w[r] = st.a[r], st.base[r] = kShift - kNone;
             st.l[r] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) st.o[r][i] = f4_t{0.f, 0.f, 0.f, 0.f};

@@ -178,3 +178,32 @@ def test_a_query_that_is_no_number_gives_none(dt, D, n, heads, x):
     assert bool(got[bad].isnan().all()) and bool(got_lse[bad].isnan().all())
     assert torch.equal(got[~bad], want[~bad]) and torch.equal(got_lse[~bad], want_lse[~bad])
     assert bool((got[n:] == 0).all()) and not bool(want.isnan().any())
+
+
+@pytest.mark.parametrize("D,n,heads,length", [(128, 1, 4, 1), (64, 1, 4, 300), (128, 5, 8, 300), (128, 70, 8, 300), (128, 280, 128, 300), (64, 200, 64, 300),
+                                              (128, 1, 8, 9000)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("exponent,scale", [(3, 0.1), (18, 0.1), (19, 0.1), (21, 0.1), (25, 0.1), (40, 0.1), (90, 0.1), (118, 0.1), (0, 1e9), (-60, 1e30)])
+def test_scores_of_any_size(D, n, heads, length, sign, exponent, scale):
+    """One key is far the best of every row, by more than any rounding: the output is its value's, bit for bit, however large the scores
+    are, of either sign; their logarithm is the best one's."""
+    best = 7 if length > 7 else 0
+    c = Cache([length], 2, D, 64, BF, seed=9)
+    pattern = torch.randint(0, 2, (D,), generator=torch.Generator().manual_seed(2)) * 2.0 - 1
+    size = 1.5 + torch.rand((length, 2, 1), generator=torch.Generator().manual_seed(3))
+    size[best] = 4.0 if sign > 0 else 0.75
+    c.k[0] = (size * pattern).to(BF)
+    c.fill_all()
+    q = (sign * 2.0 ** exponent * pattern).to(BF).expand(n, heads, D).contiguous().cuda()
+    ws = scap.KV4Workspace(c.cache, seqs=1, tokens=n, heads=heads)
+    lse = torch.empty((n, heads), device="cuda")
+    got = scap.kv4_attention(c.cache, q, i32([0, n]), c.d_table, c.d_lens, scale=scale, lse=lse, workspace=ws).cpu()
+    k, v = c.stood_for(0)
+    want = torch.from_numpy(v[best].astype(np.float16)).to(BF).repeat_interleave(heads // 2, 0)
+    assert torch.equal(got, want.expand_as(got)), (got.float() - want.float()).abs().max()
+    z = scale * sign * 2.0 ** exponent * (k @ pattern.double().numpy())     # [length, 2]
+    top = np.sort(z, 0)[::-1]
+    assert length == 1 or (top[0] - top[1] > 25).all(), "exp(-25) of length values moves no bit of them"
+    want_lse = torch.from_numpy(z[best]).repeat_interleave(heads // 2)
+    # keys carry 2^-11 each, the scale and its logarithm's base 2^-24 each
+    assert bool(((lse.cpu().double() - want_lse).abs() <= 1.01 * 2.0 ** -11 * want_lse.abs() + 1e-4).all())
