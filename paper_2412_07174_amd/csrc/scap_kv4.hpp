@@ -138,4 +138,12 @@ __device__ __forceinline__ Kv4Span kv4_span(const Kv4Seqs& s, int P, int b) {
     return {a, e - a, len};
 }
 
+// Two values rounded to nearest even.
+__device__ __forceinline__ uint32_t round16(float x, float y, int dt) {
+    typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
+    typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+    if (dt == kBF16) return __builtin_bit_cast(uint32_t, b2_t{(__bf16)x, (__bf16)y});
+    return __builtin_bit_cast(uint32_t, h2_t{(_Float16)x, (_Float16)y});
+}
+
 }  // namespace scap

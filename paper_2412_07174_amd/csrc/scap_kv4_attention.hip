@@ -576,13 +576,6 @@ __device__ __forceinline__ int first_channel(int quarter, int e) {
     return D == 64 ? 8 * (o & 7) + 4 * (o >> 3) : 8 * o;
 }
 
-// two values rounded to nearest even
-__device__ __forceinline__ uint32_t round16(float x, float y, int dt) {
-    typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
-    if (dt == kBF16) return __builtin_bit_cast(uint32_t, b2_t{(__bf16)x, (__bf16)y});
-    return as_u32(h2_t{(_Float16)x, (_Float16)y});
-}
-
 // N channels of one finished row
 template <int N>
 __device__ __forceinline__ void store_row(const Kv4AttnArgs& a, const Work& w, int row, int d, const float* x) {

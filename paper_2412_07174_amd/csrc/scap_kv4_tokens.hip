@@ -190,18 +190,6 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(Kv4TokensArgs a) {
     }
 }
 
-namespace {
-
-// Two values rounded to the output's type.
-__device__ __forceinline__ uint32_t round16(float x, float y, int dt) {
-    typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
-    typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
-    if (dt == kBF16) return __builtin_bit_cast(uint32_t, b2_t{(__bf16)x, (__bf16)y});
-    return __builtin_bit_cast(uint32_t, h2_t{(_Float16)x, (_Float16)y});
-}
-
-}  // namespace
-
 template <int D, int NT>
 __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4TokensArgs a) {
     constexpr int LPV = D / 8, LPU = 2 * LPV;
