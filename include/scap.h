@@ -392,7 +392,7 @@ int scap_kv4_attention(const scap_kv4_cache* cache, int64_t layer, const void* q
 
 /*
  * ASYNC.  Pages for sequences that grow from old_lens to new_lens (DEVICE int32 [B]; nothing to do where not larger).  Pages past the
- * old length are dropped first (tokens that were cut off), so that rows end where their length says.  A partly filled
+ * old length are dropped first (tokens that were cut off): up to the first slot without one, and in every slot that the new length takes.  A partly filled
  * last page that other rows hold too is replaced by a copy of its own, in all layers: in the order of the sequences, the last
  * holder keeps the page.  All or nothing: where pages are missing no row gets any.
  *   info       DEVICE  int32 [4]: pages missing (0: done; -1: a new length beyond S pages), pages taken, how many of them copies,

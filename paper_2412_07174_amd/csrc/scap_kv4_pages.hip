@@ -72,10 +72,22 @@ __global__ __launch_bounds__(kPlanThreads) void kv4_reserve_plan_kernel(Kv4Pool 
     for (int b = tid; b < B; b += kPlanThreads) {
         const int o = max(old_lens[b], 0), n = new_lens[b];
         int32_t* row = table + (int64_t)b * S;
-        // pages past the old length (a block of drafted tokens that was cut, say) leave before any are taken
-        for (int s = (int)(((int64_t)o + P - 1) >> p.lgP); s < S && row[s] != -1; ++s) {
-            if ((uint32_t)row[s] < (uint64_t)p.pages) atomicSub(&p.refs[row[s]], 1);
-            row[s] = -1;
+        // Pages past the old length (a block of drafted tokens that was cut, say) leave before any are taken: those up to the first slot that
+        // names none, and all in slots that the new length takes.
+        const int taken = n > o ? (n - 1) >> p.lgP : -1;
+        constexpr int FLY = 4;
+        bool more = true;
+        for (int s = (int)(((int64_t)o + P - 1) >> p.lgP); s < S && more; s += FLY) {
+            int32_t e[FLY];
+#pragma unroll
+            for (int u = 0; u < FLY; ++u) e[u] = s + u < S ? row[s + u] : -1;
+#pragma unroll
+            for (int u = 0; u < FLY; ++u) {
+                more = more && (e[u] != -1 || s + u <= taken);
+                if (!more || e[u] == -1) continue;
+                if ((uint32_t)e[u] < (uint64_t)p.pages) atomicSub(&p.refs[e[u]], 1);
+                row[s + u] = -1;
+            }
         }
         if (n > cap) s_over = 1;
     }

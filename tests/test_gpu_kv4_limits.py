@@ -207,3 +207,37 @@ def test_scores_of_any_size(D, n, heads, length, sign, exponent, scale):
     want_lse = torch.from_numpy(z[best]).repeat_interleave(heads // 2)
     # keys carry 2^-11 each, the scale and its logarithm's base 2^-24 each
     assert bool(((lse.cpu().double() - want_lse).abs() <= 1.01 * 2.0 ** -11 * want_lse.abs() + 1e-4).all())
+
+
+@pytest.mark.parametrize("old,new", [(50, 130), (50, 97), (48, 200), (0, 256), (3, 4), (130, 131), (50, 50)])
+def test_a_row_cut_before_what_its_window_kept_loses_no_page(old, new):
+    """refs stays the number of entries that name a page, whatever gap lies between the new end and what is left behind it."""
+    P, S = 16, 16
+    cache = scap.KV4Cache(40, 1, 64, page_tokens=P)
+    ws = scap.KV4Workspace(cache, seqs=2)
+    table = torch.full((2, S), -1, dtype=torch.int32, device="cuda")
+    assert scap.kv4_reserve(cache, table, i32([0, 0]), i32([200, 30]), workspace=ws).tolist() == [0, 15, 0, 25]
+    scap.kv4_free(cache, table, keep_from=i32([100, 0]))
+    kept = table[0].clone()
+    assert kept.tolist()[:6] == [-1] * 6 and kept[6:13].min() >= 0
+    info = scap.kv4_reserve(cache, table, i32([old, 30]), i32([new, 30]), workspace=ws).tolist()
+    rows = table.cpu().numpy()
+    assert np.array_equal(np.bincount(rows[rows >= 0], minlength=40), cache.refs.cpu().numpy())
+    assert info[0] == 0 and info[3] == int((cache.refs == 0).sum())
+    if new > old:   # every slot that the new tokens take has a page of its own
+        mine = rows[0, old // P:-(-new // P)]
+        assert (mine >= 0).all() and len(set(rows[rows >= 0].tolist())) == (rows >= 0).sum()
+
+
+def test_the_drop_of_a_long_cut_end():
+    """More pages behind the old length than are looked at together, up to the row's end."""
+    for S in (1, 2, 3, 4, 5, 7, 8, 9, 33):
+        cache = scap.KV4Cache(S + 1, 1, 64, page_tokens=16)
+        ws = scap.KV4Workspace(cache, seqs=1)
+        for keep in range(0, S + 1, 3):
+            cache.refs.zero_()
+            table = torch.full((1, S), -1, dtype=torch.int32, device="cuda")
+            scap.kv4_reserve(cache, table, i32([0]), i32([16 * S]), workspace=ws)
+            before = table.clone()
+            assert scap.kv4_reserve(cache, table, i32([16 * keep]), i32([16 * keep]), workspace=ws).tolist() == [0, 0, 0, S + 1 - keep]
+            assert torch.equal(table[:, :keep], before[:, :keep]) and bool((table[:, keep:] == -1).all()) and int(cache.refs.sum()) == keep
