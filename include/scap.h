@@ -316,10 +316,11 @@ int scap_read_probe(const void* src, size_t bytes, uint32_t* out, void* stream);
  *     value scales [P/4][D/32][2][4] fp16    s of four tokens, then their c
  * A code q of 0..15 stands for s * (q + 64) + c.  For a group x of 32 channels of one token:
  *     s = fp16((max x - min x) / 15),   c = fp16(min x - 64 s),   q = clamp(rint((x - c) / s) - 64, 0, 15)   (0 where s = 0)
- * with every operation one IEEE fp32 operation.  Where a head's key or value of a token holds a NaN or an infinity, or a
- * group whose s, c or 79 s + c (what code 15 stands for, rounded once to fp16) is none in fp16, the token cannot be read for that head: its
- * codes are 0 and all its scales, key and value, are NaN.  A query that sees such a token gets NaN; no other does.  So every value that can
- * be read is one of fp16's range, which attention widens it to; a pool that was not filled by scap_kv4_append has to keep to that.
+ * with every operation one IEEE fp32 operation, its result rounded to fp16 after that, and -0 less than 0.  Where a head's key or value of a
+ * token holds a NaN or an infinity, or a group whose s, c or 79 s + c (what code 15 stands for, rounded once to fp16) is none in fp16, the token
+ * cannot be read for that head: its codes are 0 and all its scales, key and value, are NaN.  A query that sees such a token gets NaN; no other
+ * does.  So every value that can be read is one of fp16's range, which attention widens it to; a pool that was not filled by
+ * scap_kv4_append has to keep to that.
  *
  * Sequences are named by three DEVICE arrays that the caller owns:
  *     table   int32 [B, S]    page of every P tokens of a sequence; -1 (or anything outside the pool): none

@@ -84,7 +84,10 @@ __device__ __forceinline__ float over_group(float v) {
     return v;
 }
 
+// An fp32 result, rounded to fp16.  It stays one of fp32 first: the compiler would round an fma once, straight to fp16, which is another number where
+// the two roundings meet in a tie (15.5 of fp16's smallest, an exact quotient of two bf16 values, say).
 __device__ __forceinline__ uint32_t f16_bits(float f) {
+    asm("" : "+v"(f));
     const _Float16 h = (_Float16)f;
     return __builtin_bit_cast(uint16_t, h);
 }

@@ -241,3 +241,69 @@ def test_the_drop_of_a_long_cut_end():
             before = table.clone()
             assert scap.kv4_reserve(cache, table, i32([16 * keep]), i32([16 * keep]), workspace=ws).tolist() == [0, 0, 0, S + 1 - keep]
             assert torch.equal(table[:, :keep], before[:, :keep]) and bool((table[:, keep:] == -1).all()) and int(cache.refs.sum()) == keep
+
+
+# ------------------------------------------------------------------------------------------------ the quantiser's roundings
+def tied(dt, n, heads, groups, seed):
+    """Groups [n, heads, groups * 32] whose range is 15 times a number that lies midway between two of fp16, exactly: their quotient in fp32 is the
+    tie itself, and any other way to round it to fp16 tells."""
+    rng = np.random.default_rng(seed)
+    shape = (n, heads, groups)
+    e = rng.integers(-25 if dt == BF else -24, -4, shape)
+    t = 2 * rng.integers(1024, 2048, shape) + 1                      # 12 bits, the last one set
+    if dt == BF:
+        small = e == -25                                             # below fp16's normal range fewer bits make a tie
+        t = np.where(small, 2 * rng.integers(0, 1024, shape) + 1, t)
+    r = 15 * t
+    keep = 8 if dt == BF else 11
+    drop = np.maximum(np.floor(np.log2(r)).astype(np.int64) + 1 - keep, 0)
+    hi = r >> drop << drop
+    lo = hi - r                                                      # as many bits as the kind has, or fewer
+    x = lo[..., None] + rng.random(shape + (32,)) * r[..., None]
+    x[..., 5], x[..., 17] = lo, hi
+    x = torch.from_numpy(np.ldexp(x, e[..., None]).astype(np.float32)).to(dt).float()
+    scaled = lambda a: torch.from_numpy(np.ldexp(a.astype(np.float64), e).astype(np.float32))[..., None]
+    x = torch.minimum(torch.maximum(x, scaled(lo)), scaled(hi))
+    assert torch.equal(x.to(dt).float(), x)
+    return x.reshape(n, heads, groups * 32).to(dt)
+
+
+def scattered(dt, n, heads, groups, seed):
+    """Groups of any size, some far from zero, some with members of very different size."""
+    rng = np.random.default_rng(seed)
+    size = np.exp2(rng.uniform(-26, 9, (n, heads, groups, 1)))
+    x = rng.standard_normal((n, heads, groups, 32)) * size
+    x += np.where(rng.random((n, heads, groups, 1)) < 0.3, size * rng.uniform(-60, 60, (n, heads, groups, 1)), 0)
+    x *= np.where(rng.random((n, heads, groups, 1)) < 0.3, np.exp2(rng.uniform(-20, 0, x.shape)), 1)
+    return torch.from_numpy(x.reshape(n, heads, groups * 32).astype(np.float32)).to(dt)
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("D,n", [(64, 1000), (128, 4032)])
+@pytest.mark.parametrize("make", [tied, scattered])
+def test_append_rounds_as_defined(dt, D, n, make):
+    """Scales and codes of many groups, bit for bit."""
+    P, heads = 64, 4
+    pages = -(-n // P)
+    k, v = make(dt, n, heads, D // 32, 1), make(dt, n, heads, D // 32, 2)
+    cache = scap.KV4Cache(pages, heads, D, page_tokens=P)
+    cache.pool.zero_()
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None].contiguous()
+    scap.kv4_append(cache, k.cuda(), v.cuda(), i32([0, n]), table, i32([n]))
+    pool = cache.pool[0].cpu().numpy()
+    tokens = lambda a: a.transpose(0, 2, 1, *range(3, a.ndim)).reshape(pages * P, heads, -1)[:n]
+    kc = pool[:, :, :P * D // 2].reshape(pages, heads, P, D // 2)
+    vc = pool[:, :, P * D // 2:P * D].reshape(pages, heads, P // 4, D // 8, 4, 4).transpose(0, 1, 2, 4, 3, 5).reshape(pages, heads, P, D // 2)
+    ks = np.ascontiguousarray(pool[:, :, P * D:P * D * 9 // 8]).view(np.uint16).reshape(pages, heads, P, D // 32, 2)
+    vs = np.ascontiguousarray(pool[:, :, P * D * 9 // 8:]).view(np.uint16).reshape(pages, heads, P // 4, D // 32, 2, 4)
+    vs = vs.transpose(0, 1, 2, 5, 3, 4).reshape(pages, heads, P, D // 32, 2)
+    qk, sk, ck, qv, sv, cv = token_codes(k.float().numpy(), v.float().numpy())
+    for codes, scales, q, s, c, x in ((kc, ks, qk, sk, ck, k), (vc, vs, qv, sv, cv, v)):
+        # -0 counts as less than 0, which numpy's minimum does not tell; c is the least member where s is 0
+        g = x.float().reshape(n, heads, D // 32, 32).numpy()
+        least = np.where(((g == 0) & np.signbit(g)).any(-1), np.float16(-0.0), np.float16(0.0))
+        c = np.where((s == 0) & (g.min(-1) == 0), least, c)
+        assert np.array_equal(tokens(scales[..., 0]), s.view(np.uint16)), "s"
+        assert np.array_equal(tokens(scales[..., 1]), c.view(np.uint16)), "c"
+        codes = tokens(codes)
+        assert np.array_equal(codes & 15, q[..., 0::2]) and np.array_equal(codes >> 4, q[..., 1::2]), "codes"
