@@ -164,7 +164,7 @@ const char* scap_status_string(int status) {
         case SCAP_ERR_SHAPE: return "shape out of range or N not a multiple of the vector width";
         case SCAP_ERR_DTYPE: return "unknown or unsupported dtype / estimator code";
         case SCAP_ERR_ALIGN: return "device pointer not 16-byte aligned";
-        case SCAP_ERR_VALUE: return "tau negative or NaN, m not finite, or sparsity outside [0,1)";
+        case SCAP_ERR_VALUE: return "a value that the call does not take: tau negative or NaN, m not finite, sparsity outside [0,1); scale not finite or not > 0, window without causal, overlapping arrays";
         case SCAP_ERR_WORKSPACE: return "workspace missing or too small";
         case SCAP_ERR_HIP: return "HIP runtime error";
         case SCAP_ERR_UNIMPL: return "not implemented in this build";

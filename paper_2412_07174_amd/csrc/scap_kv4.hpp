@@ -7,11 +7,12 @@
 //   value scales [P/4][D/32][2][4] fp16    s of four tokens, then their c
 // Each part is laid out as the attention kernel's lanes take it (scap_kv4_attention.hip): the keys' product contracts over channels, so a
 // lane holds channels of one token; the values' contracts over tokens, so a lane holds four tokens of one channel octet.
-// Appending a token touches whole words only, so tokens appended in one call never share one.
+// Codes and key scales are whole words of a token's own.  Its value scales are single halves of words that its neighbours share, written
+// with 2-byte stores: tokens of one call, of different workgroups, lie side by side there, so such a word is never read, changed and written back.
 //
 // A code q stands for s * (q + 64) + c.  The offset makes widening one instruction: a nibble put into bits 4-7 of the fp16
 // 64.0 is 64 + q exactly, and one packed fp16 fma gives the value.  c, the value of code -64, is rounded to fp16: it moves
-// the grid by at most 64 s * 2^-11 = s / 32 where the group is centred (more, as any fp16 offset, where it lies far from 0).
+// the grid by at most |c| * 2^-11: 0.035 s where the group is centred (c = -71.5 s), more, as any fp16 offset, where it lies far from 0.
 #pragma once
 
 #include "scap_device.hpp"

@@ -4,9 +4,10 @@
 //
 // A kv head's G query heads and a sequence's new tokens are the rows r of one product.  A wavefront takes RT tiles of 16 rows and walks over 32
 // tokens at a time; both products are formed transposed, S^T = K Q^T and O^T = V^T P^T, with the 16 x 16 x 32 fp16 matrix
-// instruction.  So the probabilities leave the first product in the very lanes that the second takes them from, and both
-// cache operands come straight from memory: the contraction order of each is the order in which a lane's words lie in a
-// block.  Nothing but the queries is shared between lanes, and no LDS is touched inside the loop.
+// instruction.  So the probabilities leave the first product in the very lanes that the second takes them from, and a lane takes
+// both cache operands as its words lie in a block: that is the order in which each product contracts.  Up to 16 rows, and more while they are
+// few, the operands stay in registers and the loop touches no LDS; blocks of 256 rows widen 64 tokens at a time into LDS for
+// all eight wavefronts (Stage).
 //
 // Widening: value = s (q + 64) + c, one bit-field insert and half a packed fp16 fma per value.  Roundings to 16 bits, all of them fp16
 // and all relative 2^-11 or less: a widened key or value (the exact one has 18 bits), a query (scaled by a power of two per row
@@ -14,8 +15,10 @@
 // [2^-14, 2^15]: 2^kShift times the usual one).  Sums, maxima and the running state are fp32.
 //
 // What bounds it: with one row tile the read of the cache, once there is enough of it (16 sequences of 32768 tokens, 8 heads of 128 channels:
-// 113 us, 5.9 TB/s), else a chain of eight dependent trips to memory (905 tokens: 9.5 us); with many rows the instructions beside
-// the products -- widening, exponentials -- with two wavefronts a SIMD to overlap them (prompts of 2048: 79 us, 0.64 PFLOP/s).
+// 114 us, 5.9 TB/s), else a chain of eight dependent trips to memory (905 tokens: 9.5 us).  With many rows the steps of the longest
+// block, one behind the other (prompts of 2048 and 1409 tokens: 32 steps of 64 tokens where a place has 25 on average; 79 us, 0.64 PFLOP/s),
+// and in a step products and vector instructions that two wavefronts a SIMD, which meet at a barrier, hardly overlap: each is busy about a
+// quarter of the time, LDS 15 %.
 #include <type_traits>
 
 #include "scap_gemv_parts.hpp"
