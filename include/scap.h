@@ -386,7 +386,8 @@ int scap_kv4_read(const scap_kv4_cache* cache, int64_t layer, void* k_out, void*
  *   max_new    the most new tokens of a sequence, 0 if not known: a hint that picks the faster kernel; results are right without it.
  *   scale      finite and > 0.  Scores scale * q . k may have any size that fp32 holds (times log2 e).
  *   out        DEVICE  [T, heads, D], dtype dt, 16-byte aligned.  Rows of tokens that belong to no sequence are not written.
- *   lse        DEVICE  fp32 [T, heads] or NULL: log of the sum of exp(scale * q . k_j); -inf where nothing is seen.
+ *   lse        DEVICE  fp32 [T, heads] or NULL: log of the sum of exp(scale * q . k_j), of the probabilities as they are used, rounded to fp16 each (2^-11);
+ *              -inf where nothing is seen.
  *   workspace  scap_kv4_workspace_bytes(cache, B, T, heads, max_new) bytes, initialised.
  */
 int scap_kv4_attention(const scap_kv4_cache* cache, int64_t layer, const void* q, int64_t q_stride_token,

@@ -307,3 +307,22 @@ def test_append_rounds_as_defined(dt, D, n, make):
         assert np.array_equal(tokens(scales[..., 1]), c.view(np.uint16)), "c"
         codes = tokens(codes)
         assert np.array_equal(codes & 15, q[..., 0::2]) and np.array_equal(codes >> 4, q[..., 1::2]), "codes"
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("D,n", [(64, 1), (128, 40)])
+def test_values_and_scales_below_fp16s_normal_range(dt, D, n):
+    """Nothing is flushed: one token's value of that size comes back as its fp16 number, whose place in the output's type it has."""
+    seqs, heads = 60, 2
+    c = Cache([1] * seqs, heads, D, 16, dt, seed=5)
+    size = torch.exp2(-torch.linspace(10, 24, seqs))
+    for b in range(seqs):
+        c.v[b] = (c.v[b].float() * size[b]).to(dt)
+        c.k[b] = (c.k[b].float() * size[b]).to(dt)
+    c.fill_all()
+    news = [n] * seqs                                   # the last of a sequence's new tokens sees its one token
+    ws = scap.KV4Workspace(c.cache, seqs=seqs, tokens=n * seqs, heads=2 * heads)
+    q = torch.randn((n * seqs, 2 * heads, D), generator=torch.Generator().manual_seed(3)).to(dt).cuda()
+    out = scap.kv4_attention(c.cache, q, i32(np.cumsum([0] + news)), c.d_table, c.d_lens, workspace=ws)[n - 1::n].cpu()
+    want = np.stack([c.stood_for(b)[1][0] for b in range(seqs)]).repeat(2, 1)
+    assert torch.equal(out, torch.from_numpy(want.astype(np.float16)).to(dt)) and bool((out != 0).any(-1).all())
