@@ -2,9 +2,9 @@
 //
 // What a pool holds is described by refs[page] alone -- the number of table entries that name the page, 0 = free -- and an allocation takes
 // the lowest free pages in the order of the call's sequences.  So no list lives between calls, every result is a function of the
-// arguments, and a call can be recorded into a graph.  The price is one scan of refs per allocation, by one workgroup: 5 us for 16 rows and 128
-// pages, 7 us for 128 rows and 1024 pages, most of it dependent trips to memory.  Copies run at 5-6 TB/s in and out (31 MB of shared last
-// pages in 11 us).
+// arguments, and a call can be recorded into a graph.  The price is one scan of refs per allocation, by one workgroup: 5 us for 8 rows and 128
+// pages, 8 us for 128 rows and 1024 pages, most of it dependent trips to memory.  Copies run at 4-5 TB/s in and out (28 MB of shared last
+// pages in 13 us, 44 MB to the front in 18).
 #include "scap_kv4.hpp"
 
 namespace scap {

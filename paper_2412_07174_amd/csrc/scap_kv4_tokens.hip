@@ -1,6 +1,6 @@
 // Filling the 4-bit cache (append) and reading it back.  Both move a token of one kv head with D/8 lanes per vector, 16 bytes a lane: a group
 // of 32 channels is four neighbouring lanes, whose minimum and maximum take two lane permutations each.  Bound by instructions and latency:
-// 12297 tokens of 8 heads of 128 channels 19 us in (2.6 + 0.8 TB/s), 15 us out; 16 tokens 3.5 us each way, three trips to memory.
+// 12297 tokens of 8 heads of 128 channels 19.6 us in (2.6 + 0.8 TB/s), 15 us out; 16 tokens 3.3 us in, 2.9 out, three trips to memory.
 #include "scap_kv4.hpp"
 
 namespace scap {
